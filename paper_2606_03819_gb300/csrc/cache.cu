@@ -36,30 +36,31 @@ __device__ __forceinline__ Change change_of(const CacheShape& c, int len, int de
     return x;
 }
 
-__device__ __forceinline__ int warp_incl_scan(int v) {
+// Sums over the sequences are of 64 bits: 4096 sequences may ask for 2^27 pages each.
+__device__ __forceinline__ long long warp_incl_scan(long long v) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, v, o);
+        const long long t = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += t;
     }
     return v;
 }
 
 // Exclusive prefix of v over the block's threads, and the block's total. All threads call it.
-__device__ int block_excl_scan(int v, int* warp_sums, int* total) {
+__device__ long long block_excl_scan(long long v, long long* warp_sums, long long* total) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
-    const int incl = warp_incl_scan(v);
+    const long long incl = warp_incl_scan(v);
     if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
     if (warp == 0) {
-        const int w = lane < n_warps ? warp_sums[lane] : 0;
-        const int s = warp_incl_scan(w);
+        const long long w = lane < n_warps ? warp_sums[lane] : 0;
+        const long long s = warp_incl_scan(w);
         if (lane < n_warps) warp_sums[lane] = s - w;
         if (lane == 31) warp_sums[32] = s;
     }
     __syncthreads();
-    const int out = warp_sums[warp] + incl - v;
+    const long long out = warp_sums[warp] + incl - v;
     *total = warp_sums[32];
     __syncthreads();
     return out;
@@ -81,14 +82,15 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(CacheShape c, tf_pla
     const int32_t *seq_len = p.seq_len, *delta = p.delta;
     int32_t *table = p.block_table, *free_list = p.free_list;
     const int extra = p.extra, width = p.slot_map ? p.width : 0x7fffffff;
-    __shared__ int warp_sums[33];
+    __shared__ long long warp_sums[33];
     const int tid = threadIdx.x, lane = tid & 31;
     // f(table entry, place in the pool) for the n pages of a lane's sequence s from its j-th on, whose places fall from `at`
-    auto each_page = [&](int s, int j, int n, int at, auto f) {
+    auto each_page = [&](int s, int j, int n, long long at, auto f) {
         if (n > 0) f(table + static_cast<size_t>(s) * c.max_pages + j, at);
         for (uint32_t more = __ballot_sync(0xffffffffu, n > 1); more; more &= more - 1) {
             const int who = __ffs(more) - 1, s2 = __shfl_sync(0xffffffffu, s, who), j2 = __shfl_sync(0xffffffffu, j, who);
-            const int n2 = __shfl_sync(0xffffffffu, n, who), at2 = __shfl_sync(0xffffffffu, at, who);
+            const int n2 = __shfl_sync(0xffffffffu, n, who);
+            const long long at2 = __shfl_sync(0xffffffffu, at, who);
             for (int i = 1 + lane; i < n2; i += 32) f(table + static_cast<size_t>(s2) * c.max_pages + j2 + i, at2 - i);
         }
     };
@@ -97,9 +99,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(CacheShape c, tf_pla
 
     // pages given back: the i-th of them (in the order of sequences and tokens) goes to place held + R - 1 - i, so
     // that taking as many pages again meets them in the same order
-    int n_back = 0;
+    long long n_back = 0;
     for (int s0 = 0; s0 < c.b; s0 += kPlanThreads) {
-        int back = 0, total;
+        int back = 0;
+        long long total;
         if (s0 + tid < c.b) {
             const Change x = change_of(c, seq_len[s0 + tid], delta[s0 + tid], extra, width);
             back = max(x.have - x.need, 0);
@@ -108,16 +111,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(CacheShape c, tf_pla
         n_back += total;
     }
     if (n_back > 0) {
-        int done = 0;
+        long long done = 0;
         for (int s0 = 0; s0 < c.b; s0 += kPlanThreads) {
-            int back = 0, need = 0, total;
+            int back = 0, need = 0;
+            long long total;
             if (s0 + tid < c.b) {
                 const Change x = change_of(c, seq_len[s0 + tid], delta[s0 + tid], extra, width);
                 back = max(x.have - x.need, 0);
                 need = x.need;
             }
-            const int order = block_excl_scan(back, warp_sums, &total);
-            each_page(s0 + tid, need, back, held + n_back - 1 - (done + order), [&](int32_t* entry, int at) {
+            const long long order = block_excl_scan(back, warp_sums, &total);
+            each_page(s0 + tid, need, back, held + n_back - 1 - (done + order), [&](int32_t* entry, long long at) {
                 if (at < c.n_pages) free_list[at] = *entry;       // more pages than the pool has: nowhere to put them
                 *entry = -1;
             });
@@ -125,32 +129,33 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(CacheShape c, tf_pla
             __syncthreads();
         }
     }
-    const int pool = min(held + n_back, c.n_pages);
+    const int pool = static_cast<int>(min(held + n_back, static_cast<long long>(c.n_pages)));
 
     // pages taken: sequence s is served if its pages and those of the sequences before it are there
-    int asked = 0, taken = 0;
+    long long asked = 0, taken = 0;
     for (int s0 = 0; s0 < c.b; s0 += kPlanThreads) {
         const int s = s0 + tid;
         Change x{0, 0, 0, 0, 0};
-        int more = 0, total;
+        int more = 0;
+        long long total;
         if (s < c.b) {
             x = change_of(c, seq_len[s], delta[s], extra, width);
             more = max(x.need - x.have, 0);
         }
-        const int order = asked + block_excl_scan(more, warp_sums, &total);
+        const long long order = asked + block_excl_scan(more, warp_sums, &total);
         const bool served = more == 0 || order + more <= pool;
         const int n_taken = served ? more : 0;
         if (s < c.b) {
             p.new_len[s] = served ? x.want : x.len;
             p.dev_status[s] = x.status | (served ? 0 : TF_DEV_POOL_EMPTY);
         }
-        each_page(s, x.have, n_taken, pool - 1 - order, [&](int32_t* entry, int at) { *entry = free_list[at]; });
-        int total_taken;
+        each_page(s, x.have, n_taken, pool - 1 - order, [&](int32_t* entry, long long at) { *entry = free_list[at]; });
+        long long total_taken;
         block_excl_scan(n_taken, warp_sums, &total_taken);
         asked += total;
         taken += total_taken;
     }
-    if (tid == 0) *p.free_count = pool - taken;
+    if (tid == 0) *p.free_count = static_cast<int>(pool - taken);
     if (slots_too) {
         __syncthreads();                                  // table, lengths and status are the block's own writes
         for (int i = tid; i < c.b * width; i += kPlanThreads) p.slot_map[i] = slot_of(c, p, i / width, i % width, added_to(p, i / width), p.new_len[i / width]);
