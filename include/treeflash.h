@@ -414,7 +414,7 @@ typedef struct {
     int32_t head_dim;     /* a multiple of 16, 16..256 */
     int32_t page;         /* tokens per page: 16, 32, 64 or 128 */
     int32_t n_pages;      /* pages of the pool, n_pages * page < 2^31 */
-    int32_t max_pages;    /* entries per sequence of the block table, max_pages * page < 2^31 */
+    int32_t max_pages;    /* entries per sequence of the block table, max_pages * page <= 2^31 - 1024 */
     int32_t dtype;        /* tf_dtype of queries, new keys and values, and the output */
 } tf_cache_dims;
 

@@ -24,7 +24,7 @@ struct AttnSplit {
 };
 
 __device__ __forceinline__ int attn_len(const AttnArgs& a, int s) {
-    const int cap = a.c.max_pages << a.c.page_log2;   // the host has checked that this fits
+    const int cap = a.c.max_pages << a.c.page_log2;   // 2^31 - 1024 at most: what follows may round it up and look ahead
     return min(max(a.seq_len[s], 0), cap);
 }
 

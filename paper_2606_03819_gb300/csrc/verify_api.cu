@@ -20,8 +20,10 @@ tf_status check_cache(const tf_cache_dims* dims, CacheShape* o) {
     int log2 = 0;
     while ((1 << log2) < d.page && log2 < 8) ++log2;
     if ((1 << log2) != d.page || d.page < 16 || d.page > 128) return TF_ERR_UNSUPPORTED;
-    const long long top = (1ll << 31) - 1;
-    if (static_cast<long long>(d.n_pages) * d.page > top || static_cast<long long>(d.max_pages) * d.page > top)
+    // Slots (page * tokens + place) and places in a sequence are int32. The attention kernels round a sequence's length up to
+    // their tiles and look up to two tiles of 128 tokens ahead, which has to fit too.
+    const long long top = (1ll << 31) - 1, longest = (1ll << 31) - 1024;
+    if (static_cast<long long>(d.n_pages) * d.page > top || static_cast<long long>(d.max_pages) * d.page > longest)
         return TF_ERR_UNSUPPORTED;
     *o = CacheShape{d.batch, d.heads, d.kv_heads, d.heads / d.kv_heads, d.head_dim, d.page, log2, d.n_pages, d.max_pages,
                     d.dtype};
