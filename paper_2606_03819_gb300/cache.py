@@ -7,14 +7,23 @@ free pages, all allocated once with torch on the target device. A speculative st
 
 `attend` sees the tokens cached before the step and the drafted nodes' own keys and values; `grow` makes room for the
 accepted path and `append` quantises it into its pages. Nothing here synchronises; `status` does.
+
+Everything that a call does - its kernels, and the tensors that it makes where none are passed - happens on the stream
+that it is given (none: the current one), so a tensor that it returns belongs to that stream. Calls of one cache have
+to be ordered among each other, as calls on one stream are: they share the lengths, the pages and one workspace.
 """
 from __future__ import annotations
 
 import math
+from contextlib import nullcontext
 
 import torch
 
 from . import binding as B
+
+
+def _on(stream):
+    return nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class PagedCache:
@@ -41,14 +50,16 @@ class PagedCache:
         """Change the lengths by delta + extra (delta = accept_len and extra = 1 for an accepted path) and return the
         new tokens' slots [batch, width]; a sequence that cannot grow keeps its length (plan_status) and has none."""
         if slot_map is None and width > 0:
-            slot_map = torch.empty((self.dims.batch, width), dtype=torch.int32, device=self.seq_len.device)
+            with _on(stream):
+                slot_map = torch.empty((self.dims.batch, width), dtype=torch.int32, device=self.seq_len.device)
         B.tf_cache_plan(self.dims, self.seq_len, delta, extra, self.block_table, self.free_list, self.free_count, slot_map,
                         self.seq_len, self.plan_status, stream)
         return slot_map
 
     def release(self, which, stream=None):
         """Empty the sequences where `which` [batch] is true: their pages return to the pool."""
-        self.grow(torch.where(which, -self.seq_len, 0), stream=stream)
+        with _on(stream):
+            self.grow(torch.where(which, -self.seq_len, 0), stream=stream)
 
     def append(self, layer: int, k, v, slot_map, src=None, stream=None):
         B.tf_cache_append(self.dims, k, v, slot_map, src, self.k[layer], self.v[layer], self.k_scale[layer],
@@ -57,15 +68,17 @@ class PagedCache:
     def attend(self, layer: int, q, k, v, mask=None, scale=None, out=None, lse=None, stream=None):
         """Attention of the new tokens over the cache and over themselves; returns out [batch, n, heads, head_dim]."""
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            with _on(stream):
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         B.tf_tree_attention(self.dims, q, k, v, self.k[layer], self.v[layer], self.k_scale[layer], self.v_scale[layer],
                             self.block_table, self.seq_len, mask, scale if scale is not None else 1 / math.sqrt(self.dims.head_dim),
                             out, lse, self.dev_status, self.ws, stream)
         return out
 
-    def status(self) -> int:
+    def status(self, stream=None) -> int:
         """Synchronise and return the TF_DEV_* flags of the last `grow` and of every `append` and `attend` so far."""
         flags = 0
-        for word in torch.cat([self.plan_status, self.dev_status]).tolist():
-            flags |= word
+        with _on(stream):
+            for word in torch.cat([self.plan_status, self.dev_status]).tolist():
+                flags |= word
         return flags
