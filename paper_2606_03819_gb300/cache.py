@@ -8,6 +8,9 @@ free pages, all allocated once with torch on the target device. A speculative st
 `attend` sees the tokens cached before the step and the drafted nodes' own keys and values; `grow` makes room for the
 accepted path and `append` quantises it into its pages. Nothing here synchronises; `status` does.
 
+A sequence that `grow` refuses keeps its length and has no slots, while its new tokens may already be drawn: who goes on
+with it has to look at plan_status (the last change's words) or at `status`, which keeps every refusal.
+
 Everything that a call does - its kernels, and the tensors that it makes where none are passed - happens on the stream
 that it is given (none: the current one), so a tensor that it returns belongs to that stream. Calls of one cache have
 to be ordered among each other, as calls on one stream are: they share the lengths, the pages and one workspace.
@@ -48,12 +51,15 @@ class PagedCache:
 
     def grow(self, delta, extra: int = 0, width: int = 0, slot_map=None, stream=None):
         """Change the lengths by delta + extra (delta = accept_len and extra = 1 for an accepted path) and return the
-        new tokens' slots [batch, width]; a sequence that cannot grow keeps its length (plan_status) and has none."""
+        new tokens' slots [batch, width]; a sequence that cannot grow keeps its length and has none: plan_status says why until
+        the next change, `status` until `clear_status`."""
         if slot_map is None and width > 0:
             with _on(stream):
                 slot_map = torch.empty((self.dims.batch, width), dtype=torch.int32, device=self.seq_len.device)
         B.tf_cache_plan(self.dims, self.seq_len, delta, extra, self.block_table, self.free_list, self.free_count, slot_map,
                         self.seq_len, self.plan_status, stream)
+        with _on(stream):
+            self.dev_status.bitwise_or_(self.plan_status)     # the next change overwrites plan_status
         return slot_map
 
     def release(self, which, stream=None):
@@ -76,9 +82,15 @@ class PagedCache:
         return out
 
     def status(self, stream=None) -> int:
-        """Synchronise and return the TF_DEV_* flags of the last `grow` and of every `append` and `attend` so far."""
+        """Synchronise and return the TF_DEV_* flags of every call since the cache was made or `clear_status` was called; those
+        of a single sequence are in dev_status."""
         flags = 0
         with _on(stream):
             for word in torch.cat([self.plan_status, self.dev_status]).tolist():
                 flags |= word
         return flags
+
+    def clear_status(self, stream=None):
+        with _on(stream):
+            self.plan_status.zero_()
+            self.dev_status.zero_()

@@ -57,3 +57,15 @@ def test_what_a_call_makes_itself_is_made_on_the_stream_it_is_given(Bn, cache, m
             call(**kw)
             assert made and all(x is want for x in made) and current == [None]
     assert len(ran) == 6 and all(a[-1] is s for a in ran[::2]) and all(a[-1] is None for a in ran[1::2])
+
+
+def test_every_refusal_stays_in_the_status(Bn, cache, monkeypatch):
+    # a plan overwrites its words: here the first one refuses two sequences, those after it none
+    words = iter([[0, Bn.TF_DEV_POOL_EMPTY, Bn.TF_DEV_BAD_LENGTH], [0, 0, 0], [0, 0, 0]])
+    monkeypatch.setattr(Bn, "tf_cache_plan", lambda *a: a[9].copy_(torch.tensor(next(words), dtype=torch.int32)))
+    cache.grow(torch.zeros(3, dtype=torch.int32))
+    cache.grow(torch.zeros(3, dtype=torch.int32))
+    cache.release(torch.ones(3, dtype=torch.bool))
+    assert cache.status() == Bn.TF_DEV_POOL_EMPTY | Bn.TF_DEV_BAD_LENGTH
+    cache.clear_status()
+    assert cache.status() == 0

@@ -61,3 +61,23 @@ def test_a_side_stream_while_the_current_one_is_busy(Bn):
         assert torch.equal(getattr(plain, name), getattr(other, name)), name
     n = plain.free_count.item()
     assert torch.equal(plain.free_list[:n], other.free_list[:n])
+
+
+def test_a_refusal_is_kept_until_it_is_cleared(Bn):
+    cache = _cache(Bn, n_pages=5)
+    t = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache.grow(t(40, 16, 1), width=40)                        # 3 + 1 pages; the fifth is the last one's
+    assert cache.status() == 0
+    cache.grow(t(1, 1, 16), width=16)                         # a page each for the second and the third: none is left
+    assert cache.plan_status.tolist() == [0, Bn.TF_DEV_POOL_EMPTY, Bn.TF_DEV_POOL_EMPTY]
+    assert cache.seq_len.tolist() == [41, 16, 1]
+    cache.grow(t(0, 0, 0))
+    cache.grow(t(1, 0, 200), width=16)                        # longer than the slot map
+    cache.release(torch.tensor([True, False, False], device="cuda"))
+    assert cache.plan_status.tolist() == [0, 0, 0]
+    assert cache.dev_status.tolist() == [0, Bn.TF_DEV_POOL_EMPTY, Bn.TF_DEV_POOL_EMPTY | Bn.TF_DEV_BAD_LENGTH]
+    assert cache.status() == Bn.TF_DEV_POOL_EMPTY | Bn.TF_DEV_BAD_LENGTH
+    cache.clear_status()
+    assert cache.status() == 0
+    cache.grow(t(1, 1, 16), width=16)                         # the released pages serve them now
+    assert cache.status() == 0 and cache.seq_len.tolist() == [1, 17, 17]
