@@ -422,7 +422,8 @@ _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
 
 
 # The checks below are written out in one condition per call: a function call for each tensor would cost as much as the
-# checks. Where the condition fails, _take finds the tensor that is to blame.
+# checks. Where the condition fails, _take finds the tensor that is to blame. Every tensor lies on the GPU that the call's
+# kernels run on, the current one: they would read another pointer as it is.
 
 def _take(name: str, t: torch.Tensor, dtype, shape) -> int:
     """Data pointer of a contiguous tensor of this type and shape."""
@@ -448,11 +449,18 @@ def _take_rows(name: str, t: torch.Tensor, dtype, batch: int, heads: int, head_d
     return n, row
 
 
-def _blame(*wants):
+def _blame_device(*tensors):
+    for name, t in tensors:
+        if t is not None and (t.get_device() < 0 or t.get_device() != torch.cuda.current_device()):
+            raise ValueError(f"{name}: expected a tensor on the current CUDA device, got one on {t.device}")
+    raise ValueError("inconsistent tensors")
+
+
+def _blame(*wants, rows=()):
     for name, t, dtype, shape in wants:
         if t is not None:
             _take(name, t, dtype, shape)
-    raise ValueError("inconsistent tensors")
+    _blame_device(*rows, *((name, t) for name, t, _, _ in wants))
 
 
 def tf_cache_plan(dims: CacheDims, seq_len, delta, extra: int, block_table, free_list, free_count, slot_map, new_len,
@@ -467,7 +475,11 @@ def tf_cache_plan(dims: CacheDims, seq_len, delta, extra: int, block_table, free
             block_table.shape == table and free_list.shape == pool and free_count.shape == (1,) and
             seq_len.is_contiguous() and delta.is_contiguous() and block_table.is_contiguous() and free_list.is_contiguous() and
             new_len.is_contiguous() and dev_status.is_contiguous() and
-            (slot_map is None or slot_map.dtype is _I32 and slot_map.shape == (dims.batch, width) and slot_map.is_contiguous())):
+            (gpu := seq_len.get_device()) >= 0 and delta.get_device() == gpu and block_table.get_device() == gpu and
+            free_list.get_device() == gpu and free_count.get_device() == gpu and new_len.get_device() == gpu and
+            dev_status.get_device() == gpu and gpu == torch.cuda.current_device() and
+            (slot_map is None or slot_map.dtype is _I32 and slot_map.shape == (dims.batch, width) and slot_map.is_contiguous() and
+             slot_map.get_device() == gpu)):
         _blame(("seq_len", seq_len, _I32, b), ("delta", delta, _I32, b), ("block_table", block_table, _I32, table),
                ("free_list", free_list, _I32, pool), ("free_count", free_count, _I32, (1,)), ("new_len", new_len, _I32, b),
                ("dev_status", dev_status, _I32, b), ("slot_map", slot_map, _I32, (dims.batch, width)))
@@ -494,10 +506,13 @@ def tf_cache_append(dims: CacheDims, k, v, slot_map, src, k_cache, v_cache, k_sc
             k_scale.shape == scales and v_scale.shape == scales and dev_status.shape == dims.per_seq and
             slot_map.is_contiguous() and k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and
             v_scale.is_contiguous() and dev_status.is_contiguous() and
-            (src is None or src.dtype is _I32 and src.shape == slots and src.is_contiguous())):
+            (gpu := k.get_device()) >= 0 and v.get_device() == gpu and slot_map.get_device() == gpu and k_cache.get_device() == gpu and
+            v_cache.get_device() == gpu and k_scale.get_device() == gpu and v_scale.get_device() == gpu and
+            dev_status.get_device() == gpu and gpu == torch.cuda.current_device() and
+            (src is None or src.dtype is _I32 and src.shape == slots and src.is_contiguous() and src.get_device() == gpu)):
         _blame(("slot_map", slot_map, _I32, slots), ("src", src, _I32, slots), ("k_cache", k_cache, _U8, pages),
                ("v_cache", v_cache, _U8, pages), ("k_scale", k_scale, _F32, scales), ("v_scale", v_scale, _F32, scales),
-               ("dev_status", dev_status, _I32, dims.per_seq))
+               ("dev_status", dev_status, _I32, dims.per_seq), rows=(("k", k), ("v", v)))
     args = _APPEND.pack(k.data_ptr(), v.data_ptr(), k_row, v_row, slot_map.data_ptr(), 0 if src is None else src.data_ptr(),
                         k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), dev_status.data_ptr(), n,
                         slots[1])
@@ -538,13 +553,17 @@ def tf_tree_attention(dims: CacheDims, q, k, v, k_cache, v_cache, k_scale, v_sca
             out.shape == (b, n, hq, hd) and k_cache.is_contiguous() and v_cache.is_contiguous() and
             k_scale.is_contiguous() and v_scale.is_contiguous() and block_table.is_contiguous() and
             seq_len.is_contiguous() and dev_status.is_contiguous() and out.is_contiguous() and
-            (mask is None or mask.dtype is _U8 and mask.shape == (b, n, n) and mask.is_contiguous()) and
-            (lse is None or lse.dtype is _F32 and lse.shape == (b, n, hq) and lse.is_contiguous()) and
+            (gpu := q.get_device()) >= 0 and k.get_device() == gpu and v.get_device() == gpu and k_cache.get_device() == gpu and
+            v_cache.get_device() == gpu and k_scale.get_device() == gpu and v_scale.get_device() == gpu and
+            block_table.get_device() == gpu and seq_len.get_device() == gpu and dev_status.get_device() == gpu and
+            out.get_device() == gpu and ws.get_device() == gpu and gpu == torch.cuda.current_device() and
+            (mask is None or mask.dtype is _U8 and mask.shape == (b, n, n) and mask.is_contiguous() and mask.get_device() == gpu) and
+            (lse is None or lse.dtype is _F32 and lse.shape == (b, n, hq) and lse.is_contiguous() and lse.get_device() == gpu) and
             ws.dtype is _U8 and ws.is_contiguous()):
         _blame(("k_cache", k_cache, _U8, pages), ("v_cache", v_cache, _U8, pages), ("k_scale", k_scale, _F32, scales),
                ("v_scale", v_scale, _F32, scales), ("block_table", block_table, _I32, table), ("seq_len", seq_len, _I32, per_seq),
                ("mask", mask, _U8, (b, n, n)), ("out", out, dt, (b, n, hq, hd)), ("lse", lse, _F32, (b, n, hq)),
-               ("dev_status", dev_status, _I32, per_seq), ("ws", ws, _U8, ws.shape))
+               ("dev_status", dev_status, _I32, per_seq), ("ws", ws, _U8, ws.shape), rows=(("q", q), ("k", k), ("v", v)))
     args = _ATTENTION.pack(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, k_row, v_row, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(),
         v_scale.data_ptr(), block_table.data_ptr(), seq_len.data_ptr(), 0 if mask is None else mask.data_ptr(), out.data_ptr(),
@@ -570,6 +589,12 @@ def tf_sample(logits, u, tok, logp=None, temperature=None, top_k=None, top_p=Non
         0 if min_p is None else _take("min_p", min_p, _F32, seqs), _take("u", u, _F32, per_row), _take("tok", tok, _I32, per_row),
         0 if logp is None else _take("logp", logp, _F32, per_row), st[0] if rows > 1 else V, rows, V,
         TF_F32 if dt is _F32 else TF_BF16, rows_per_seq)
+    if not ((gpu := logits.get_device()) >= 0 and u.get_device() == gpu and tok.get_device() == gpu and
+            (logp is None or logp.get_device() == gpu) and (temperature is None or temperature.get_device() == gpu) and
+            (top_k is None or top_k.get_device() == gpu) and (top_p is None or top_p.get_device() == gpu) and
+            (min_p is None or min_p.get_device() == gpu) and gpu == torch.cuda.current_device()):
+        _blame_device(("logits", logits), ("u", u), ("tok", tok), ("logp", logp), ("temperature", temperature), ("top_k", top_k),
+                      ("top_p", top_p), ("min_p", min_p))
     status = load_library().tf_sample(args, _stream(stream))
     if status:
         _check("tf_sample", status)
