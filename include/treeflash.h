@@ -474,7 +474,8 @@ tf_status tf_attention_workspace_size(const tf_cache_dims* dims, int32_t n, size
  *   out[s, i, h] = sum_t p_t v_t,  p = softmax_t(scale * q[s, i, h] . k_t)
  * over every cached token t < seq_len[s] and every new token j with mask[s, i, j] != 0 (keys and values of head
  * h / (heads / kv_heads)). Values that no row may see (masked nodes, places behind seq_len) may hold anything, NaN
- * too. Scales are finite and not negative. Scores, sums and the output are accumulated in fp32. */
+ * too. Scales are finite and not negative. A query with an infinity or a NaN makes the outputs of its row NaN (unless
+ * all of its scores are -inf: then they may be 0). Scores, sums and the output are accumulated in fp32. */
 typedef struct {
     const void* q;              /* rows as in tf_cache_append, heads * head_dim contiguous elements each */
     const void* k;              /* the new tokens' keys and values, kv_heads * head_dim contiguous elements each */

@@ -518,7 +518,8 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                 const int e = static_cast<int>(amax >> 23) - 127;
                 const int shift = amax == 0 || amax >= 0x7f800000u ? 0 : max(min(7 - e, 126), -120);
                 const float up = __uint_as_float(static_cast<uint32_t>(shift + 127) << 23);
-                qmul = __uint_as_float(static_cast<uint32_t>(127 - shift) << 23) * zscale;
+                // e4m3 has no infinities, and would cut the row's large elements beside one: such a row's scores are NaN
+                qmul = amax >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 - shift) << 23) * zscale;
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) {        // four columns of hi, four of lo
                     uint32_t hi[4], lo[4];
