@@ -208,8 +208,8 @@ __global__ void __launch_bounds__(32 * kWarps) simt_attention_kernel(AttnArgs a,
             if (row >= p.rows) continue;
             const int node = row / a.c.group, head = g.h * a.c.group + (row - node * a.c.group);
             if (!attn_row_present(a, g.s, node)) m[r] = -INFINITY, l[r] = 0.0f;
+            const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
             if (whole) {
-                const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
                 const size_t at = (static_cast<size_t>(g.s) * a.n + node) * a.c.hq + head;
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(32 * kWarps) simt_attention_kernel(AttnArgs a,
                 const size_t at = static_cast<size_t>(slot) * p.rt + rr;
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
-                    if (lane + 32 * d < hd) p.part_o[at * hd + lane + 32 * d] = o[r][d];
+                    if (lane + 32 * d < hd) p.part_o[at * hd + lane + 32 * d] = l[r] == 0.0f ? 0.0f : o[r][d] * inv;
                 if (lane == 0) p.part_ml[at] = make_float2(m[r], l[r]);
             }
         }
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(32 * kWarps) simt_attention_kernel(AttnArgs a,
 }
 
 // ---- joining split items ------------------------------------------------------------------------------------------
-// Weighs each piece's numerators and sum of a row by exp2 of its maximum against the largest. Few items are cut in many
+// Weighs each piece's output of a row by its sum, times exp2 of its maximum against the largest. Few items are cut in many
 // pieces: a CTA per row then, its warps sharing the pieces (SPREAD); many items in few: a warp per row.
 // The kernel before lets this one start early, so the work is listed while that one runs: everything before it on the
 // stream has then finished, and it does not write what is read for that (seq_len).
@@ -269,8 +269,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) combine_kernel(AttnArgs a, At
         const int mine = cb + step * lane;
         if (mine <= c1) {
             const float2 ml = p.part_ml[static_cast<size_t>(2 * mine + (mine == c0)) * p.rt + rr];
-            f = ml.y == 0.0f ? 0.0f : exp2f(ml.x - base);
-            l = fmaf(ml.y, f, l);
+            f = ml.y == 0.0f ? 0.0f : ml.y * exp2f(ml.x - base);
+            l += f;
         }
         const int n = min(32, (c1 - cb) / step + 1);
         for (int j = 0; j < n; j += kAtOnce) {

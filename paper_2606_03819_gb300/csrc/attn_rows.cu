@@ -12,9 +12,13 @@
 //
 // e4m3 widens to f16 exactly. Queries are bf16 numbers times a power of two per row that puts the row's largest
 // element at 2^14..2^15: exact for elements down to 2^-24 of it, those below lose bits that are less than 2^-38
-// of the largest. A page's scale of keys multiplies the scores; its scale of values goes into the exponent,
-//   t = z + log2(v_scale),  P = 2^(t - m),  m = max t - 14,   sum of weights = sum P / v_scale,
-// so P is at most 2^14 and keeps f16's 11 bits down to 2^-28 of the largest term of the output, whatever the scales.
+// of the largest. A page's scale of keys multiplies the scores z. The weights are those of the scores alone, in fp32,
+//   w = 2^(z - m),  m the largest score so far, rounded up,   sum of weights = sum w,
+// so that the values' scales cannot make their sum overflow or vanish. For the product they take the page's scale of values and
+// are rounded to f16,
+//   P = w v_scale 2^-sh,  sh whole, such that the largest P so far is 2^13..2^14,
+// which keeps f16's 11 bits down to 2^-27 of the largest term of the output. m and sh are whole numbers: what is summed so far
+// is moved by powers of two, without rounding.
 //
 // Bounded by HBM: one token of 64 sequences with up to 32768 cached (32 heads on 8, size 128; 2.15 GB) takes 348 us, 6.2 TB/s, with
 // two CTAs per SM and 255 registers; three at 168 registers spill and take 594. One sequence with 4100 cached: 10.6 us, a chain of
@@ -34,6 +38,7 @@ constexpr int kTok = 32;                  // tokens of one warp per step: two fr
 constexpr int kTile = kTok * kWarps;      // tokens of one CTA per step
 constexpr float kLow = -1e30f;            // maximum of nothing yet
 constexpr float kHead = 14.0f;            // log2 of the largest P
+constexpr float kLeastShift = -200.0f;    // sh where no value counts yet
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -149,6 +154,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
     extern __shared__ long long prefix[];
     __shared__ __align__(16) float so[kWarps][R][HD];
     __shared__ float2 sml[kWarps][R];
+    __shared__ float ssh[kWarps][R];
     __shared__ uint8_t present[R];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 
@@ -204,20 +210,34 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
             qmul[nt][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
         }
 
-        float o[NT][MT][4], m[NT][2], l[NT][2];
+        float o[NT][MT][4], m[NT][2], sh[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            m[nt][0] = m[nt][1] = kLow, l[nt][0] = l[nt][1] = 0.0f;
+            m[nt][0] = m[nt][1] = kLow, sh[nt][0] = sh[nt][1] = kLeastShift, l[nt][0] = l[nt][1] = 0.0f;
 #pragma unroll
             for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.0f;
         }
-        auto rescale = [&](int nt, float m0, float m1) {                // raise the maxima of rows 2t, 2t + 1
-            const float f0 = ex2(m[nt][0] - m0), f1 = ex2(m[nt][1] - m1);
-            m[nt][0] = m0, m[nt][1] = m1;
-            l[nt][0] *= f0, l[nt][1] *= f1;
+        // m and sh of rows 2t, 2t + 1 for two groups of tokens: [group][row] the largest scores, log2 of the values' scale
+        auto raise = [&](int nt, const float (&top)[2][2], const float (&lv)[2]) {
+            float m2[2], kept[2], sh2[2];                               // kept: sh that leaves the numerators as they are
+            bool any = false;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                m2[r] = fmaxf(m[nt][r], ceilf(fmaxf(top[0][r], top[1][r])));
+                const float t2 = fmaxf(top[0][r] - m2[r] + lv[0], top[1][r] - m2[r] + lv[1]);
+                kept[r] = sh[nt][r] - (m2[r] - m[nt][r]);
+                sh2[r] = fmaxf(fmaxf(kept[r], ceilf(t2) - kHead), kLeastShift);
+                any |= m2[r] > m[nt][r] || sh2[r] > kept[r];
+            }
+            if (!__any_sync(0xffffffffu, any)) return;
+            const float f0 = ex2(kept[0] - sh2[0]), f1 = ex2(kept[1] - sh2[1]);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) l[nt][r] *= ex2(m[nt][r] - m2[r]), m[nt][r] = m2[r], sh[nt][r] = sh2[r];
 #pragma unroll
             for (int i = 0; i < MT; ++i) o[nt][i][0] *= f0, o[nt][i][1] *= f1, o[nt][i][2] *= f0, o[nt][i][3] *= f1;
         };
+        // what takes a weight to P (2^126 at most: beyond it, a weight of less than 2^-112 takes less)
+        auto to_p = [&](int nt, int r, float lv) { return ex2(fminf(lv - sh[nt][r], 126.0f)); };
 
         const int c_end = sg.t1 < cached_tiles ? sg.t1 : cached_tiles;
         if (sg.t0 < c_end) {
@@ -234,13 +254,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
                     page_ids(a, sg.s, tok + 2 * kTile, tile + 2 < c_end ? len : 0, pid);
                 }
                 if (cur.n[0] + cur.n[1] == 0) continue;
-                float lv[2], iv[2];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    // a scale of zero stands at 2^-100 in the exponent, and its page's weights count in the sum alone
-                    const float v = fmaxf(cur.vs[f], kMinScale);
-                    lv[f] = log2f(v), iv[f] = 1.0f / v;
-                }
+                const float lv[2] = {log2f(cur.vs[0]), log2f(cur.vs[1])};   // -inf: values of zeros
                 float s[NT][2][4];
 #pragma unroll
                 for (int f = 0; f < 2; ++f) {
@@ -257,37 +271,33 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
                 uint32_t pf[NT][2][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    float top0 = kLow, top1 = kLow;
+                    float top[2][2];
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
                         const float f0 = qmul[nt][0] * cur.ks[f], f1 = qmul[nt][1] * cur.ks[f];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const bool there = g + 8 * e < cur.n[f];
-                            const float z0 = there ? fmaf(s[nt][f][2 * e], f0, lv[f]) : -INFINITY;
-                            const float z1 = there ? fmaf(s[nt][f][2 * e + 1], f1, lv[f]) : -INFINITY;
-                            s[nt][f][2 * e] = z0, s[nt][f][2 * e + 1] = z1;
-                            top0 = fmaxf(top0, z0), top1 = fmaxf(top1, z1);
+                            s[nt][f][2 * e] = there ? s[nt][f][2 * e] * f0 : -INFINITY;
+                            s[nt][f][2 * e + 1] = there ? s[nt][f][2 * e + 1] * f1 : -INFINITY;
+                        }
+                        top[f][0] = fmaxf(s[nt][f][0], s[nt][f][2]), top[f][1] = fmaxf(s[nt][f][1], s[nt][f][3]);
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) {
+                            top[f][0] = fmaxf(top[f][0], __shfl_xor_sync(0xffffffffu, top[f][0], d));
+                            top[f][1] = fmaxf(top[f][1], __shfl_xor_sync(0xffffffffu, top[f][1], d));
                         }
                     }
-#pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) {
-                        top0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, d));
-                        top1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, d));
-                    }
-                    top0 -= kHead, top1 -= kHead;
-                    if (__any_sync(0xffffffffu, top0 > m[nt][0] || top1 > m[nt][1]))
-                        rescale(nt, fmaxf(top0, m[nt][0]), fmaxf(top1, m[nt][1]));
+                    raise(nt, top, lv);
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
-                        float w0 = 0.0f, w1 = 0.0f;
+                        const float up0 = to_p(nt, 0, lv[f]), up1 = to_p(nt, 1, lv[f]);
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float p0 = ex2(s[nt][f][2 * e] - m[nt][0]), p1 = ex2(s[nt][f][2 * e + 1] - m[nt][1]);
-                            w0 += p0, w1 += p1;
-                            pf[nt][f][e] = transpose8(cur.vs[f] > 0.0f ? pack_f16(p0, p1) : 0u);
+                            const float w0 = ex2(s[nt][f][2 * e] - m[nt][0]), w1 = ex2(s[nt][f][2 * e + 1] - m[nt][1]);
+                            l[nt][0] += w0, l[nt][1] += w1;
+                            pf[nt][f][e] = transpose8(pack_f16(w0 * up0, w1 * up1));
                         }
-                        l[nt][0] = fmaf(w0, iv[f], l[nt][0]), l[nt][1] = fmaf(w1, iv[f], l[nt][1]);
                     }
                 }
 #pragma unroll
@@ -339,10 +349,11 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
                         z[e] = see[e] ? z[e] * zscale : -INFINITY;
                     }
                     if (!__any_sync(0xffffffffu, see[0] || see[1])) continue;
-                    rescale(nt, fmaxf(m[nt][0], z[0] - kHead), fmaxf(m[nt][1], z[1] - kHead));
-                    const float p0 = ex2(z[0] - m[nt][0]), p1 = ex2(z[1] - m[nt][1]);
+                    raise(nt, {{z[0], z[1]}, {-INFINITY, -INFINITY}}, {0.0f, 0.0f});
+                    const float w0 = ex2(z[0] - m[nt][0]), w1 = ex2(z[1] - m[nt][1]);
                     // every lane of a row holds its weight; the sums are added over the lanes later
-                    if (g == 0) l[nt][0] += p0, l[nt][1] += p1;
+                    if (g == 0) l[nt][0] += w0, l[nt][1] += w1;
+                    const float p0 = w0 * to_p(nt, 0, 0.0f), p1 = w1 * to_p(nt, 1, 0.0f);
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
                         const float v0 = bf16_lo(vp[i]), v1 = bf16_hi(vp[i]);
@@ -367,7 +378,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
                 float sum = l[nt][e];
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                if (g == 0) sml[warp][8 * nt + 2 * t + e] = make_float2(m[nt][e], sum);
+                if (g == 0) sml[warp][8 * nt + 2 * t + e] = make_float2(m[nt][e], sum), ssh[warp][8 * nt + 2 * t + e] = sh[nt][e];
                 float* to = so[warp][8 * nt + 2 * t + e] + EL * g;
 #pragma unroll
                 for (int i = 0; i < MT; i += 2)
@@ -381,23 +392,29 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
             const int rr = i / (HD / 4), d = 4 * (i - rr * (HD / 4)), row = row0 + rr;
             if (row >= p.rows) continue;
             const int node = row / a.c.group, head = sg.h * a.c.group + row - node * a.c.group;
-            float mm = sml[0][rr].x, ll = 0.0f;
+            float mm = sml[0][rr].x, ll = 0.0f, top = -INFINITY, e[kWarps];
 #pragma unroll
             for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, sml[w][rr].x);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {                          // the numerators are a warp's times 2^e
+                ll = fmaf(sml[w][rr].y, ex2(sml[w][rr].x - mm), ll);
+                e[w] = ssh[w][rr] + (sml[w][rr].x - mm);
+                top = fmaxf(top, e[w]);
+            }
             float4 v = make_float4(0, 0, 0, 0);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float f = ex2(sml[w][rr].x - mm);
+                const float f = ex2(e[w] - top);
                 const float4 ov = *reinterpret_cast<const float4*>(&so[w][rr][d]);
-                ll = fmaf(sml[w][rr].y, f, ll);
                 v.x = fmaf(ov.x, f, v.x), v.y = fmaf(ov.y, f, v.y), v.z = fmaf(ov.z, f, v.z), v.w = fmaf(ov.w, f, v.w);
             }
+            const bool none = !present[rr] || ll == 0.0f;
+            const float inv = 1.0f / ll, half = ex2(0.5f * top);        // 2^top in two steps: it may pass fp32 where the output does not
+            v.x = none ? 0.0f : v.x * inv * half * half, v.y = none ? 0.0f : v.y * inv * half * half;
+            v.z = none ? 0.0f : v.z * inv * half * half, v.w = none ? 0.0f : v.w * inv * half * half;
             if (whole) {
-                const bool none = !present[rr] || ll == 0.0f;
-                const float inv = none ? 0.0f : 1.0f / ll;
                 const size_t at = (static_cast<size_t>(sg.s) * a.n + node) * a.c.hq + head;
-                const __nv_bfloat162 lo = __floats2bfloat162_rn(none ? 0.0f : v.x * inv, none ? 0.0f : v.y * inv);
-                const __nv_bfloat162 hi = __floats2bfloat162_rn(none ? 0.0f : v.z * inv, none ? 0.0f : v.w * inv);
+                const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
                 uint2 w;
                 w.x = *reinterpret_cast<const uint32_t*>(&lo), w.y = *reinterpret_cast<const uint32_t*>(&hi);
                 *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at * HD + d) = w;

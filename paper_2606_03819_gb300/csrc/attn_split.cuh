@@ -19,8 +19,8 @@ struct AttnSplit {
     int min_tiles;     // least share of a CTA, in tiles
     int ctas;          // CTAs that share the work
     int rt;            // rows per tile (of partial results)
-    float* part_o;     // [2 * ctas][rt][hd]: numerators, relative to the row's m
-    float2* part_ml;   // [2 * ctas][rt]: row maximum in the base-2 log domain, sum of exp2
+    float* part_o;     // [2 * ctas][rt][hd]: a piece's own output (numerators / sum), 0 where a row saw nothing of it
+    float2* part_ml;   // [2 * ctas][rt]: of its scores in the base-2 log domain, m (the maximum or little more) and the sum of exp2(z - m)
 };
 
 __device__ __forceinline__ int attn_len(const AttnArgs& a, int s) {

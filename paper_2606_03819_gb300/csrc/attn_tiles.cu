@@ -6,9 +6,9 @@
 // without widening a byte. A row is scaled by the power of two that puts its largest element at 2^7..2^8: 4 bits in hi and
 // the other 4 of bf16's 8 in lo, exact down to 2^-10 of the largest element, within 2^-18 of it below.
 // Output. Splitting the weights the same way costs the softmax more instructions than everything else it does, so the values
-// are widened instead (to f16, exactly), once per tile for all rows, and the weights are rounded to f16:
-// P = 2^(t - m) with t = z + log2(v_scale) as in attn_rows.cu, and m such that the largest P is 2^8..2^15: 11 bits
-// down to 2^-22 of the largest or less.
+// are widened instead (to f16, exactly), once per tile for all rows, and the weights are rounded to f16, as in attn_rows.cu:
+// w = 2^(z - m) in fp32 for their sum, P = w v_scale 2^-sh for the product, with sh such that the largest P is 2^7..2^15:
+// 11 bits down to 2^-21 of the largest or less.
 //
 // One CTA per SM takes 128 query rows against tiles of 128 tokens. Everything that the products accumulate or take per row is in
 // TMEM, all of its 512 columns: S twice, O, P and the queries. With the queries there, S needs shared memory for the
@@ -19,7 +19,7 @@
 //                from TMEM)
 //   warps 2, 3   values from e4m3 to f16; what lies behind the last token becomes 0
 //   warps 4..19  softmax: four threads per row, 32 columns of S each, which exchange their maxima through shared memory
-// O is rescaled only when a row's maximum has grown by more than 7 (in log2) since the last time.
+// O is rescaled only when a row's largest P would pass 2^15, and m moves only when a score passes it by more than 20 (in log2).
 // Bounded by the softmax warps' instructions and the chain from S to the next P: 2400 cycles per 128 rows and 128 tokens of 128
 // elements, of which the tensor cores need 1100. Trees of 65 nodes of 16 sequences with 1000 to 16384 cached, 32 heads on 8: 261 us,
 // 570 TFLOP/s of what is asked for (their 260 rows per head of keys take three tiles of 128; 64 nodes, two tiles: 194 us). Products issued by
@@ -38,6 +38,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLow = -1e30f;
 constexpr float kTop = 8.0f, kSlack = 7.0f;   // log2 of the largest P after a rescale, and its growth until the next
+constexpr float kRoom = 20.0f;                // log2 of the largest w
+constexpr float kFar = 65536.0f;              // a move of m beyond it leaves little of what was added to it
+constexpr float kLeastShift = -200.0f;        // sh where no value counts yet
 constexpr int kTile = 128;                    // tokens of a tile
 constexpr int kMaxPagesPerTile = 8;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
@@ -53,8 +56,8 @@ struct WideSplit {
     int rows, row_tiles;                      // rows of (sequence, head); items of 128 of them
     int step;                                 // sequences per listed prefix sum
     int ctas;
-    float* base_o;                            // [b * hkv * rows][hd]
-    float2* base_ml;
+    float* base_o;                            // [b * hkv * rows][hd]: a piece's own output (numerators / sum), 0 where there is none
+    float2* base_ml;                          // its m and sum of 2^(z - m)
     float* cta_o;                             // [ctas][128][hd]
     float2* cta_ml;
     unsigned long long wait_ns;
@@ -203,7 +206,7 @@ __device__ __forceinline__ bool elect_one() {
 }
 
 struct PageScale {
-    float ks, lv, iv, some;                   // keys' scale; log2 and inverse of the values'; some: 0 where that is 0
+    float ks, lv, out, unused;                // keys' scale, log2 of the values'; -inf for a page that is left out, 0 for others
 };
 
 template <int HD>
@@ -216,8 +219,8 @@ struct WideCfg {
     static constexpr int kV = kVh + VHST * kVhBytes;
     static constexpr int kScales = kV + VST * kKvBytes;
     static constexpr int kBars = kScales + SST * kMaxPagesPerTile * sizeof(PageScale);
-    static constexpr int kMax = kBars + 512;                       // [2][128][4]: maxima (sums) of a row's four threads
-    static constexpr int kPrefix = kMax + 2 * 128 * 16;
+    static constexpr int kMax = kBars + 512;                       // [2][128][4] pairs: maxima (sums) of a row's four threads
+    static constexpr int kPrefix = kMax + 2 * 128 * 32;
     static constexpr size_t smem = kPrefix + (kListed + 1) * 8 + 1024;   // 1024: alignment
 };
 static_assert(WideCfg<128>::smem <= 227 * 1024, "shared memory");
@@ -327,9 +330,8 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                 if (lane < per_tile) {
                     // the keys' buffer is free: the scores of KST tiles ago are done, the softmax has read those of two before
                     // that, and with them it had done with the scales of SST tiles ago
-                    const float v = fmaxf(my_vs, kMinScale);
                     PageScale sc;
-                    sc.ks = my_ks, sc.lv = my_pid >= 0 ? log2f(v) : -INFINITY, sc.iv = 1.0f / v, sc.some = my_vs > 0.0f ? 1.0f : 0.0f;
+                    sc.ks = my_ks, sc.lv = my_pid >= 0 ? log2f(my_vs) : -INFINITY, sc.out = my_pid >= 0 ? 0.0f : -INFINITY, sc.unused = 0.0f;
                     scales[sst * kMaxPagesPerTile + lane] = sc;
                 }
                 const int pages = __popc(__ballot_sync(0xffffffffu, my_pid >= -1));   // pages of this tile, from the first on
@@ -436,7 +438,7 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                 // a lane keeps its piece of the row and goes down the rows
                 const int c = tid % PIECES, r0 = tid / PIECES;
                 bool all = valid == kTile;
-                for (int k = 0; k < kTile >> a.c.page_log2; ++k) all &= sc[k].some != 0.0f;
+                for (int k = 0; k < kTile >> a.c.page_log2; ++k) all &= sc[k].lv > -INFINITY;
                 if (all) {
 #pragma unroll
                     for (int i0 = 0; i0 < EACH; i0 += 8) {
@@ -451,7 +453,7 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                     for (int i = 0; i < EACH; ++i) {
                         const int r = r0 + i * (64 / PIECES);
                         uint4 w = make_uint4(0, 0, 0, 0);
-                        if (r < valid && sc[r >> a.c.page_log2].some != 0.0f) w = *reinterpret_cast<const uint4*>(from + swizzled<HD>(r, c));
+                        if (r < valid && sc[r >> a.c.page_log2].lv > -INFINITY) w = *reinterpret_cast<const uint4*>(from + swizzled<HD>(r, c));
                         widen(r, c, w);
                     }
                 }
@@ -467,23 +469,27 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
         const int rr = (warp & 3) * 32 + lane;            // row of the tile = TMEM lane
         const uint32_t lane_at = tmem + (static_cast<uint32_t>(warp & 3) * 32 << 16);
         const uint32_t s_col = lane_at + C::kS + 32 * part, p_col = lane_at + C::kP + 16 * part, o_col = lane_at + C::kO + part * (HD / 4);
-        float* slots = reinterpret_cast<float*>(smem + C::kMax) + rr * 4;
+        float2* slots = reinterpret_cast<float2*>(smem + C::kMax) + rr * 4;
         uint64_t* meet = meet4 + (warp & 3);
         uint32_t met = 0;
         // what the row's four threads have in place of v: posted, then taken when something else has been done
-        auto post = [&](float v) {
+        auto post = [&](float2 v) {
             slots[(met & 1) * 128 * 4 + part] = v;
             ptx::mbar_arrive(meet);
         };
-        auto take = [&](float4* all) -> bool {
+        auto take = [&](float4 (&all)[2]) -> bool {
             const bool got = wait(meet, met);
-            *all = *reinterpret_cast<const float4*>(slots + (met & 1) * 128 * 4);
+            all[0] = *reinterpret_cast<const float4*>(slots + (met & 1) * 128 * 4);
+            all[1] = *reinterpret_cast<const float4*>(slots + (met & 1) * 128 * 4 + 2);
             ++met;
             return got;
         };
         auto exchange = [&](float v, float4* all) -> bool {
-            post(v);
-            return take(all);
+            float4 two[2];
+            post(make_float2(v, 0.0f));
+            const bool got = take(two);
+            *all = make_float4(two[0].x, two[0].z, two[1].x, two[1].z);
+            return got;
         };
         const float zscale = a.scale * kLog2e;
         uint32_t it = 0;                                  // tiles of the CTA so far
@@ -541,11 +547,14 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                 ptx::tc_fence_before();
             }
             ptx::mbar_arrive(q_full);
-            float m = kLow, l = 0.0f;
+            float m = 0.0f, room = -INFINITY;             // room: the score from which on m moves (at first any)
+            float sh = kLeastShift, l = 0.0f;
             uint32_t r[32];                               // this thread's part of the scores
             int valid = 0;                                // tokens there, from the first on
-            float f[2], lv[2], iv[2];                     // of its two groups of 16 tokens: factor of the scores, log2 and inverse of the values' scale
-            // S of a tile into registers, and the largest score that this thread has of it to the row's other threads
+            // of its two groups of 16 tokens: factor of the scores, log2 of the values' scale, -inf for a page that is left out
+            float f[2], lv[2], out[2];
+            // S of a tile into registers, and to the row's other threads the largest score that this thread has of it and, relative
+            // to m, log2 of the largest product of a weight with a scale of values
             auto load = [&](uint32_t i, int t) -> bool {
                 if (!(wait(s_full + (i & 1), i >> 1) && wait(sc_full + i % SST, i / SST))) return false;
                 if (!rows_here) {
@@ -563,7 +572,7 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                     for (int e = 0; e < 32; ++e)
                         if (e >= valid) r[e] = 0xff800000u;            // -inf, whatever stood there
                 }
-                float top = kLow;
+                float z2[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const uint32_t* z = r + 16 * k;
@@ -573,23 +582,38 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                     mx = fmaxf(mx, __uint_as_float(z[15]));
                     const PageScale s = sc[(32 * part + 16 * k) >> a.c.page_log2];
                     const bool none = 16 * k >= valid;                 // beyond the last page there is no scale
-                    f[k] = none ? 1.0f : qmul * s.ks, lv[k] = none ? 0.0f : s.lv, iv[k] = none ? 0.0f : s.iv;
-                    top = fmaxf(top, fmaf(mx, f[k], lv[k]));           // (-inf where there is none)
+                    f[k] = none ? 1.0f : qmul * s.ks, lv[k] = none ? 0.0f : s.lv;
+                    z2[k] = __fmul_rn(mx, f[k]) + (none ? 0.0f : s.out);   // (-inf where there is none)
+                    out[k] = none ? 0.0f : s.out;
                 }
-                post(top);
+                post(make_float2(fmaxf(z2[0], z2[1]), fmaxf(z2[0] - m + lv[0], z2[1] - m + lv[1])));
                 return true;
             };
             ok = load(it, g.t0);
             for (int t = g.t0; t < g.t1 && ok; ++t, ++it) {
                 if (rows_here) {
-                    float4 all;
-                    ok = take(&all);
+                    float4 all[2];
+                    ok = take(all);
                     if (!ok) break;
-                    const float top = max3(fmaxf(all.x, all.y), all.z, all.w) - kTop;
-                    if (__any_sync(0xffffffffu, top > m + kSlack)) {
-                        // this row's P would pass 2^15: its maximum moves, and what it has goes down
-                        const float m2 = top > m + kSlack ? top : m, down = ex2(m - m2);
-                        m = m2, l *= down;
+                    const float top = fmaxf(max3(all[0].x, all[0].z, all[1].x), all[1].z);
+                    float p_top = fmaxf(max3(all[0].y, all[0].w, all[1].y), all[1].w);
+                    if (__any_sync(0xffffffffu, top > room || p_top > sh + (kTop + kSlack))) {
+                        if (top > room) {
+                            // the numerators, relative to 2^(m + sh), stay as they are
+                            const float m2 = ceilf(top), up = m2 - m;
+                            l *= ex2(-up), sh -= up, p_top -= up;
+                            if (fabsf(up) > kFar) {
+                                p_top = -INFINITY;                     // nothing is left of it: the largest of the tile's scales bounds it
+                                const int pages = (min(g.len - t * kTile, kTile) + a.c.page - 1) >> a.c.page_log2;
+#pragma unroll 1
+                                for (int k = 0; k < pages; ++k) p_top = fmaxf(p_top, scales[it % SST * kMaxPagesPerTile + k].lv);
+                            }
+                            m = m2, room = m + kRoom;
+                        }
+                        // where P would pass 2^15, what this row has goes down
+                        const bool moves = p_top > sh + (kTop + kSlack) || sh < kLeastShift;
+                        const float sh2 = moves ? fmaxf(ceilf(p_top) - kTop, kLeastShift) : sh, down = ex2(sh - sh2);
+                        sh = sh2;
                         if (t > g.t0) {
                             ok = wait(p_free, it - 1);                 // O belongs to the products of the tile before
                             if (!ok) break;
@@ -607,12 +631,13 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                     uint32_t w[16];                       // 32 weights
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float b = lv[k] - m;
-                        const unsigned long long f2 = f2_pack(f[k], f[k]), b2 = f2_pack(b, b);
+                        // (2^126 at most: a weight that would take more is less than 2^-111)
+                        const float b = out[k] - m, up = ex2(fminf(lv[k] - sh, 126.0f));
+                        const unsigned long long f2 = f2_pack(f[k], f[k]), b2 = f2_pack(b, b), up2 = f2_pack(up, up);
                         float pr[16];
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
-                            const unsigned long long arg = f2_fma(f2_pack(__uint_as_float(r[16 * k + i]), __uint_as_float(r[16 * k + i + 1])), f2, b2);
+                            const unsigned long long arg = f2_add(f2_mul(f2_pack(__uint_as_float(r[16 * k + i]), __uint_as_float(r[16 * k + i + 1])), f2), b2);
                             pr[i] = ex2(f2_lo(arg)), pr[i + 1] = ex2(f2_hi(arg));
                         }
                         if (valid < 32) {
@@ -623,10 +648,11 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                         unsigned long long sum = f2_pack(pr[0], pr[1]);
 #pragma unroll
                         for (int i = 2; i < 16; i += 2) sum = f2_add(sum, f2_pack(pr[i], pr[i + 1]));
-                        l = fmaf(f2_lo(sum) + f2_hi(sum), iv[k], l);
+                        l += f2_lo(sum) + f2_hi(sum);
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
-                            const __half2 h = __floats2half2_rn(pr[i], pr[i + 1]);
+                            const unsigned long long p2 = f2_mul(f2_pack(pr[i], pr[i + 1]), up2);
+                            const __half2 h = __floats2half2_rn(f2_lo(p2), f2_hi(p2));
                             w[8 * k + i / 2] = *reinterpret_cast<const uint32_t*>(&h);
                         }
                     }
@@ -654,14 +680,18 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
             float4 all;
             ok = exchange(l, &all);
             if (!ok) break;
-            // this piece's numerators and sums
+            // this piece's output and sum
+            const float sum = (all.x + all.y) + (all.z + all.w);
             const size_t at = g.t0 > 0 ? static_cast<size_t>(blockIdx.x) * 128 + rr : (static_cast<size_t>(g.s) * a.c.hkv + g.h) * p.rows + row;
             float* o = (g.t0 > 0 ? p.cta_o : p.base_o) + at * HD + part * (HD / 4);
-            if (row < p.rows && part == 0) (g.t0 > 0 ? p.cta_ml : p.base_ml)[at] = make_float2(m, (all.x + all.y) + (all.z + all.w));
+            if (row < p.rows && part == 0) (g.t0 > 0 ? p.cta_ml : p.base_ml)[at] = make_float2(sum == 0.0f ? kLow : m, sum);
+            const float inv = 1.0f / sum, half = ex2(0.5f * sh);       // 2^sh in two steps: it may pass fp32 where the output does not
 #pragma unroll
             for (int c = 0; c < HD / 4; c += 16) {
                 uint32_t v[16];
                 ptx::tmem_ld_16cols(o_col + c, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = sum == 0.0f ? 0u : __float_as_uint(__uint_as_float(v[i]) * inv * half * half);
                 if (row < p.rows) {
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(o + c + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
@@ -990,8 +1020,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 3) join_kernel(AttnArgs a, Wi
 #pragma unroll
             for (int o2 = 1; o2 < 8; o2 <<= 1) top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, o2));
             top2 = fmaxf(top2, top);
-            const float down = ex2(top - top2), f_mine = ex2(ml.x - top2);
-            float more = ml.y * f_mine;
+            const float down = ex2(top - top2), f_mine = ml.y * ex2(ml.x - top2);
+            float more = f_mine;
 #pragma unroll
             for (int o2 = 1; o2 < 8; o2 <<= 1) more += __shfl_xor_sync(0xffffffffu, more, o2);
             top = top2, sum = fmaf(sum, down, more);
@@ -1045,9 +1075,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 3) join_kernel(AttnArgs a, Wi
             float sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float f = ex2(ml[k].x - top);
+                const float f = ml[k].y * ex2(ml[k].x - top);
                 factors[(g + 8 * e) * 16 + t + 4 * k] = f;
-                sum = fmaf(ml[k].y, f, sum);
+                sum += f;
             }
             if (t == 0) factors[(g + 8 * e) * 16 + 8] = down;
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from test_verifier_gpu import _attend, _setup
+from test_verifier_gpu import _attend, _check, _setup
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +40,44 @@ def test_a_query_that_is_not_finite_gives_nan_in_its_row_alone(Bn, n, dtype, val
     rest = torch.ones_like(lse, dtype=torch.bool)
     rest[:, i, 2] = False
     assert torch.equal(out[rest], want[rest]) and torch.equal(lse[rest], want_lse[rest])
+
+
+@pytest.mark.parametrize("n", FEW_AND_MANY)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lift", [-60, 0, 45, 100])
+def test_pages_of_zeros_beside_values_of_any_scale(Bn, n, dtype, lift):
+    # a page whose values are all zero has the scale that an append gives it, 2^-100; its tokens count in the sum as any others
+    c = _setup(Bn, lens=[90, 160], n=n, heads=8, kv_heads=2, hd=64, page=16, dtype=dtype, seed=22, v_std=2.0 ** lift, nan_tail=False)
+    c["vc"][::2], c["vs"][::2] = 0, 2.0 ** -100
+    out, lse, status = _attend(Bn, c)
+    assert not status.any()
+    _check(c, out, lse)
+
+
+@pytest.mark.parametrize("n", [1, 20])
+def test_long_contexts_of_zeros(Bn, n):
+    # keys and values of zeros, as a padded head has them: 32768 tokens of weight 1, and the new tokens, of whose keys the last row's
+    # own alone meets its query, with a weight of 32768. Pieces of the work hold all of a sequence's cached tokens.
+    b, hq, hkv, hd, page, length = 64, 8, 8, 64, 128, 32768
+    pages = length // page
+    d = Bn.CacheDims(batch=b, heads=hq, kv_heads=hkv, head_dim=hd, page=page, n_pages=b * pages, max_pages=pages)
+    z = lambda *s, dt=torch.uint8: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+    kc, vc = z(b * pages, hkv, page, hd), z(b * pages, hkv, page, hd)
+    ks = torch.full((b * pages, hkv), 2.0 ** -100, device="cuda")
+    table = torch.arange(b * pages, dtype=torch.int32, device="cuda").view(b, pages)
+    lens = torch.full((b,), length, dtype=torch.int32, device="cuda")
+    q, k, v = (z(b, n, h, hd, dt=torch.bfloat16) for h in (hq, hkv, hkv))
+    q[:, -1, :, 0], k[:, -1, :, 0] = 1.0, 1.0
+    v[:, -1] = 3.0
+    scale = math.log(length)                                  # a score of log 32768
+    out, lse, status = z(b, n, hq, hd, dt=torch.bfloat16), z(b, n, hq, dt=torch.float32), z(b, dt=torch.int32)
+    Bn.tf_tree_attention(d, q, k, v, kc, vc, ks, ks.clone(), table, lens, None, scale, out, lse, status, Bn.alloc_attention_workspace(d, n))
+    torch.cuda.synchronize()
+    assert not status.any()
+    seen = length + torch.arange(1, n + 1, dtype=torch.float64)   # tokens of weight 1
+    seen[-1] += length - 1
+    # sums of 32768 terms in fp32, and one weight of a score of 10
+    assert (lse.cpu().double() - seen.log()[None, :, None]).abs().max() <= (length + 16) * 2.0 ** -24
+    want = torch.zeros(n, dtype=torch.float64)
+    want[-1] = 3.0 * length / seen[-1]
+    assert (out.cpu().double() - want[None, :, None, None]).abs().max() <= 3.0 * 2.0 ** -8
