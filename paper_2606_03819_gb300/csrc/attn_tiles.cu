@@ -601,7 +601,8 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                         if (top > room) {
                             // the numerators, relative to 2^(m + sh), stay as they are
                             const float m2 = ceilf(top), up = m2 - m;
-                            l *= ex2(-up), sh -= up, p_top -= up;
+                            p_top -= up;
+                            if (room > -INFINITY) l *= ex2(-up), sh -= up;     // (nothing was added to it before)
                             if (fabsf(up) > kFar) {
                                 p_top = -INFINITY;                     // nothing is left of it: the largest of the tile's scales bounds it
                                 const int pages = (min(g.len - t * kTile, kTile) + a.c.page - 1) >> a.c.page_log2;

@@ -1,10 +1,12 @@
 """Attention over the paged cache at the edges of its numbers."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
-from test_verifier_gpu import _attend, _check, _setup
+from oracle import verifier_oracle as VO
+from test_verifier_gpu import _attend, _check, _np, _oracle, _setup
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +83,32 @@ def test_long_contexts_of_zeros(Bn, n):
     want = torch.zeros(n, dtype=torch.float64)
     want[-1] = 3.0 * length / seen[-1]
     assert (out.cpu().double() - want[None, :, None, None]).abs().max() <= 3.0 * 2.0 ** -8
+
+
+def _equal_scores(Bn, n, dtype, length, power):
+    """Every key is the same, so that every score is -2^power times the row's own factor and every weight 1: the output is the mean of
+    the values and lse the score, whatever page and scale a token lies in."""
+    c = _setup(Bn, lens=[length, max(length - 7, 0)], n=n, heads=8, kv_heads=2, hd=64, page=16, dtype=dtype, seed=23, mask="causal", nan_tail=False)
+    d = c["dims"]
+    c["kc"][:], c["ks"][:] = VO.to_e4m3(np.float64(1.0)), 2.0 ** -3
+    c["qkv"][:, :, :d.heads] = -1.0 - 0.25 * torch.arange(d.heads)[:, None] / d.heads
+    c["qkv"][:, :, d.heads:d.heads + d.kv_heads] = 2.0 ** -3
+    c["scale"] = 2.0 ** (power - 3)                           # 64 products of 2^-3 each
+    out, lse, status = _attend(Bn, c)
+    assert not status.any()
+    o, l, mag, _ = _oracle(c)
+    terms = length + n
+    # equal scores have equal weights in any arithmetic that rounds them alike; the rest are the sums, a weight's rounding and the output's.
+    # A score is a sum of head_dim products in fp32.
+    r = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -23
+    tol = mag * (r + (2 * terms + 16) * 2.0 ** -24) + r * np.abs(o)
+    assert (np.abs(_np(out) - o) <= tol).all(), float((np.abs(_np(out) - o) / tol).max())
+    assert (np.abs(_np(lse) - l) <= (d.head_dim + 16) * 2.0 ** -24 * np.abs(l) + (terms + 16) * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("n", FEW_AND_MANY)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [0, 40, 300])
+@pytest.mark.parametrize("power", [7, 10])
+def test_rows_whose_scores_are_all_far_below_zero(Bn, n, dtype, length, power):
+    _equal_scores(Bn, n, dtype, length, power)
