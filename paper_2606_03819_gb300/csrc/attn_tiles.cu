@@ -172,6 +172,12 @@ __device__ __forceinline__ void tmem_st_4cols(uint32_t taddr, const uint32_t* r)
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Sums rounded toward zero, which no product before them is fused with: the product keeps its own rounding.
+__device__ __forceinline__ unsigned long long f2_add_rz(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -638,7 +644,7 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
                         float pr[16];
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
-                            const unsigned long long arg = f2_add(f2_mul(f2_pack(__uint_as_float(r[16 * k + i]), __uint_as_float(r[16 * k + i + 1])), f2), b2);
+                            const unsigned long long arg = f2_add_rz(f2_mul(f2_pack(__uint_as_float(r[16 * k + i]), __uint_as_float(r[16 * k + i + 1])), f2), b2);
                             pr[i] = ex2(f2_lo(arg)), pr[i + 1] = ex2(f2_hi(arg));
                         }
                         if (valid < 32) {
