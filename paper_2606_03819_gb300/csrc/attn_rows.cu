@@ -36,7 +36,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWarps = 4;
 constexpr int kTok = 32;                  // tokens of one warp per step: two fragments of 16
 constexpr int kTile = kTok * kWarps;      // tokens of one CTA per step
-constexpr float kLow = -1e30f;            // maximum of nothing yet
+constexpr float kLow = -3.402823466e38f;  // maximum of nothing yet: no finite score is below it
 constexpr float kHead = 14.0f;            // log2 of the largest P
 constexpr float kLeastShift = -200.0f;    // sh where no value counts yet
 
@@ -278,8 +278,9 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const bool there = g + 8 * e < cur.n[f];
-                            s[nt][f][2 * e] = there ? s[nt][f][2 * e] * f0 : -INFINITY;
-                            s[nt][f][2 * e + 1] = there ? s[nt][f][2 * e + 1] * f1 : -INFINITY;
+                            // (rounded, so that a large score cannot differ from its maximum)
+                            s[nt][f][2 * e] = there ? __fmul_rn(s[nt][f][2 * e], f0) : -INFINITY;
+                            s[nt][f][2 * e + 1] = there ? __fmul_rn(s[nt][f][2 * e + 1], f1) : -INFINITY;
                         }
                         top[f][0] = fmaxf(s[nt][f][0], s[nt][f][2]), top[f][1] = fmaxf(s[nt][f][1], s[nt][f][3]);
 #pragma unroll
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) rows_attention_kernel(AttnArgs
                         }
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) z[e] += __shfl_xor_sync(0xffffffffu, z[e], d);
-                        z[e] = see[e] ? z[e] * zscale : -INFINITY;
+                        z[e] = see[e] ? __fmul_rn(z[e], zscale) : -INFINITY;
                     }
                     if (!__any_sync(0xffffffffu, see[0] || see[1])) continue;
                     raise(nt, {{z[0], z[1]}, {-INFINITY, -INFINITY}}, {0.0f, 0.0f});

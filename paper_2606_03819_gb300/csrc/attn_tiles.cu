@@ -36,7 +36,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLow = -1e30f;
+constexpr float kLow = -3.402823466e38f;      // maximum of nothing yet: no finite score is below it
 constexpr float kTop = 8.0f, kSlack = 7.0f;   // log2 of the largest P after a rescale, and its growth until the next
 constexpr float kRoom = 20.0f;                // log2 of the largest w
 constexpr float kFar = 65536.0f;              // a move of m beyond it leaves little of what was added to it
@@ -879,7 +879,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 3) join_kernel(AttnArgs a, Wi
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                z[u][i] = see[u][i] ? z[u][i] * zscale : -INFINITY;
+                z[u][i] = see[u][i] ? __fmul_rn(z[u][i], zscale) : -INFINITY;
                 top[i >> 1] = fmaxf(top[i >> 1], z[u][i]);
             }
         // bf16 weights may be large: the maximum moves only where it grows by more than 8 (in log2)

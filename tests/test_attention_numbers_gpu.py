@@ -120,3 +120,11 @@ def test_rows_whose_scores_are_all_far_below_zero(Bn, n, dtype, length, power):
 @pytest.mark.parametrize("power", [20, 25])
 def test_equal_scores_where_fp32_is_coarse(Bn, n, dtype, length, power):
     _equal_scores(Bn, n, dtype, length, power)
+
+
+@pytest.mark.parametrize("n", FEW_AND_MANY)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [0, 40, 300])
+@pytest.mark.parametrize("power", [99, 101, 124])
+def test_rows_whose_scores_lie_around_and_below_minus_1e30(Bn, n, dtype, length, power):
+    _equal_scores(Bn, n, dtype, length, power)
