@@ -729,8 +729,8 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
 }
 
 // ---- new tokens, and the pieces together --------------------------------------------------------------------------
-// A warp holds 16 query rows: their attention over the new tokens by m16n8k16 bf16 products (weights rounded to
-// bf16), then the cached tokens' pieces are added in their order, and the output is written. The new tokens' keys and values
+// A warp holds 16 query rows: their attention over the new tokens by m16n8k16 bf16 products (weights in two bf16 parts, 16 bits
+// and more: one part lost a third of the output's accuracy where the new tokens are all there is), then the cached tokens' pieces are added in their order, and the output is written. The new tokens' keys and values
 // are copied to shared memory in chunks of up to 128 (a tree of the usual size is one) and the mask turned into bits, so
 // that one wait for memory covers them all. Bounded by latency.
 // Many items: a CTA's four warps take 16 rows each. Few (SPREAD): all four take the same 16 rows, each every fourth 16 of the new tokens,
@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 3) join_kernel(AttnArgs a, Wi
                 for (int i = 0; i < EL; ++i) o[i][2 * e] *= f, o[i][2 * e + 1] *= f;
             }
         }
-        uint32_t pa[4];
+        uint32_t pa[4], pb[4];                            // the weights, and what bf16 leaves of them
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float pr[4];
@@ -909,7 +909,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 3) join_kernel(AttnArgs a, Wi
                 pr[i] = see[u][i] ? ex2(z[u][i] - m[i >> 1]) : 0.0f;
                 w[i >> 1] += pr[i];
             }
-            pa[2 * u] = pack_bf16(pr[0], pr[1]), pa[2 * u + 1] = pack_bf16(pr[2], pr[3]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t h = pack_bf16(pr[2 * e], pr[2 * e + 1]);
+                pa[2 * u + e] = h, pb[2 * u + e] = pack_bf16(pr[2 * e] - bf16_lo(h), pr[2 * e + 1] - bf16_hi(h));
+            }
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) l[e] += w[e];
@@ -927,7 +931,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 3) join_kernel(AttnArgs a, Wi
 #pragma unroll
         for (int i = 0; i < EL; ++i) {
             const uint32_t sel = i & 1 ? 0x7632 : 0x5410;
-            mma_bf16_16816(o[i], pa, __byte_perm(v[0][i / 2], v[1][i / 2], sel), __byte_perm(v[2][i / 2], v[3][i / 2], sel));
+            const uint32_t b0 = __byte_perm(v[0][i / 2], v[1][i / 2], sel), b1 = __byte_perm(v[2][i / 2], v[3][i / 2], sel);
+            mma_bf16_16816(o[i], pa, b0, b1);
+            mma_bf16_16816(o[i], pb, b0, b1);
         }
         if (odd) {
             // infinities and NaN reach the rows that see them, and those alone

@@ -128,3 +128,35 @@ def test_equal_scores_where_fp32_is_coarse(Bn, n, dtype, length, power):
 @pytest.mark.parametrize("power", [99, 101, 124])
 def test_rows_whose_scores_lie_around_and_below_minus_1e30(Bn, n, dtype, length, power):
     _equal_scores(Bn, n, dtype, length, power)
+
+
+# contexts with new tokens alone, with few rows and with many
+SHAPES = [([0, 0], 64, 128), ([0], 130, 64), ([0, 0, 0], 3, 64), ([700, 130], 1, 128), ([300, 5], 4, 64), ([700, 64, 1], 33, 128), ([900], 20, 64)]
+
+
+@pytest.mark.parametrize("lens,n,hd", SHAPES)
+@pytest.mark.parametrize("mask", ["causal", "tree"])
+@pytest.mark.parametrize("q_std", [0.5, 3.0])
+def test_bf16_outputs_to_what_their_arithmetic_leaves(Bn, lens, n, hd, mask, q_std):
+    """A score is an fp32 sum of head_dim exact products, each sum cut to fp32: (hd + 16) 2^-23 of the largest sum of |q_d k_td|, with 16 for the
+    scalings, the exponential and its argument. Many rows hold their queries in two e4m3 parts over cached keys: 2^-17 of the row's
+    largest element for each element. A weight is then off by twice that, and by its rounding: f16 over cached tokens (2^-11, and
+    2^-25 absolute where the largest is 2^7 at least, times 448 scales), two bf16 parts or fp32 over new ones (2^-16). Sums of t terms
+    in fp32 lose t 2^-24 each; the output is rounded to bf16 once, 2^-8."""
+    c = _setup(Bn, lens=lens, n=n, heads=8, kv_heads=2, hd=hd, page=32, mask=mask, seed=31, q_std=q_std)
+    d = c["dims"]
+    out, lse, status = _attend(Bn, c)
+    assert not status.any()
+    o, l, mag, top = _oracle(c)
+    x = _np(c["qkv"])
+    q_top = np.abs(x[:, :, :8]).max(-1)
+    keys = np.abs(VO.from_e4m3(c["kc"]) * c["ks"][:, :, None, None]).sum(-1)
+    split = q_top * np.nanmax(keys, initial=0.0) * c["scale"] * 2.0 ** -17 if max(lens) else 0.0
+    z = (hd + 16) * 2.0 ** -23 * top + split
+    terms = max(lens) + n
+    r = (2.0 ** -11 if max(lens) else 0.0) + 2.0 ** -16
+    small = terms * 2.0 ** -32 * 448 * float(c["vs"].max()) if max(lens) else 0.0
+    tol = mag * (2 * z[..., None] + r + (2 * terms + 16) * 2.0 ** -24) + small + 2.0 ** -8 * (1 + 2.0 ** -7) * np.abs(o) + 1e-30
+    assert (np.abs(_np(out) - o) <= tol).all(), float((np.abs(_np(out) - o) / tol).max())
+    fin = np.isfinite(l)
+    assert (np.abs(_np(lse) - l)[fin] <= (2 * z + (terms + 16) * 2.0 ** -24)[fin] + 2.0 ** -22 * (1 + np.abs(l[fin]))).all()
