@@ -4,7 +4,7 @@
 // Scores. The keys' bytes are multiplied as they lie: tcgen05 takes e4m3 operands at twice bf16's rate, so the queries are
 // split in two e4m3 parts, q = hi + lo, and both products are added up in the same fp32 accumulator: the rate of bf16
 // without widening a byte. A row is scaled by the power of two that puts its largest element at 2^7..2^8: 4 bits in hi and
-// the other 4 of bf16's 8 in lo, exact down to 2^-10 of the largest element, within 2^-18 of it below.
+// the other 4 of bf16's 8 in lo, exact down to 2^-9 of the largest element and within 2^-17 of it below.
 // Output. Splitting the weights the same way costs the softmax more instructions than everything else it does, so the values
 // are widened instead (to f16, exactly), once per tile for all rows, and the weights are rounded to f16, as in attn_rows.cu:
 // w = 2^(z - m) in fp32 for their sum, P = w v_scale 2^-sh for the product, with sh such that the largest P is 2^7..2^15:

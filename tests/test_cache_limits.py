@@ -83,3 +83,19 @@ def test_tensors_on_the_host_or_another_gpu_are_refused(Bn, name, monkeypatch):
     with pytest.raises(ValueError, match="current CUDA device"):
         f(**args, stream=Null)
     assert len(reached) == 1
+
+
+def test_bits_that_two_e4m3_parts_keep_of_a_query():
+    # a row's largest element lies in [2^7, 2^8); hi is the nearest e4m3 number, lo that of the rest: every bf16 number (8 bits) below it
+    import numpy as np
+    from oracle import verifier_oracle as VO
+    worst = 0.0
+    for top in np.arange(128, 256) * 2.0 ** 7 / 128:
+        x = (np.arange(128, 256)[:, None] / 128 * 2.0 ** np.arange(-24, 8)[None, :]).ravel()
+        x = x[x <= top]
+        hi = VO.from_e4m3(VO.to_e4m3(x))
+        lo = VO.from_e4m3(VO.to_e4m3(x - hi))
+        off = np.abs(x - hi - lo)
+        assert not off[x >= top * 2.0 ** -9].any()
+        worst = max(worst, float((off / top).max()))
+    assert worst == 2.0 ** -17
