@@ -440,10 +440,11 @@ def _take_rows(name: str, t: torch.Tensor, dtype, batch: int, heads: int, head_d
     if t.dtype is not dtype or len(shape) != 4 or shape != (batch, shape[1], heads, head_dim):
         raise ValueError(f"{name}: expected {dtype} [{batch}, n, {heads}, {head_dim}], got {t.dtype} {tuple(shape)}")
     n, row = shape[1], st[1]
-    if st == (n * row, row, head_dim, 1) and (n > 1 or row >= heads * head_dim):
+    if st == (n * row, row, head_dim, 1) and (n > 1 or batch > 1 and row >= heads * head_dim):
         return n, row
-    # dimensions of one element may have any stride
-    row = row if n > 1 else st[0] if batch > 1 else max(row, heads * head_dim)
+    # dimensions of one element may have any stride, also one that rows could not have
+    if n == 1:
+        row = st[0] if batch > 1 else row if row >= heads * head_dim and row % 16 == 0 else heads * head_dim
     if (head_dim > 1 and st[3] != 1) or (heads > 1 and st[2] != head_dim) or (batch > 1 and n > 0 and st[0] != n * row):
         raise ValueError(f"{name}: rows must be contiguous and evenly spaced, got strides {st}")
     return n, row

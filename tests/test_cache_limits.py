@@ -99,3 +99,15 @@ def test_bits_that_two_e4m3_parts_keep_of_a_query():
         assert not off[x >= top * 2.0 ** -9].any()
         worst = max(worst, float((off / top).max()))
     assert worst == 2.0 ** -17
+
+
+def test_a_single_row_may_have_any_stride(Bn):
+    # the first token of a buffer whose rows are 516 elements apart: the distance to a next row, which there is not, does not matter
+    bf = torch.bfloat16
+    x = torch.zeros(1, 3, 516, dtype=bf)[..., :512].unflatten(2, (8, 64))
+    assert Bn._take_rows("q", x[:, :1], bf, 1, 8, 64) == (1, 512)
+    assert Bn._take_rows("q", x, bf, 1, 8, 64) == (3, 516)          # (refused by the library)
+    assert Bn._take_rows("q", torch.zeros(1, 1, 8, 64, dtype=bf), bf, 1, 8, 64) == (1, 512)
+    y = torch.zeros(2, 3, 1024, dtype=bf)[..., :512].unflatten(2, (8, 64))
+    assert Bn._take_rows("q", y[:, :1], bf, 2, 8, 64) == (1, 3072)
+    assert Bn._take_rows("q", torch.zeros(2, 1, 8, 64, dtype=bf), bf, 2, 8, 64) == (1, 512)
