@@ -195,6 +195,11 @@ def _stream(stream=None):
     return _current_raw_stream(torch.cuda.current_device())
 
 
+def _stream_on(stream, gpu: int):
+    """_stream for a caller that knows the current device."""
+    return _stream(stream) if stream is not None or _current_raw_stream is None else _current_raw_stream(gpu)
+
+
 def weights_struct(w: dict) -> TfWeights:
     get = w.get
     return TfWeights(*[None if (t := get(k)) is None else t.data_ptr() for k in WEIGHT_KEYS])
@@ -486,7 +491,7 @@ def tf_cache_plan(dims: CacheDims, seq_len, delta, extra: int, block_table, free
                ("dev_status", dev_status, _I32, b), ("slot_map", slot_map, _I32, (dims.batch, width)))
     args = _PLAN.pack(seq_len.data_ptr(), delta.data_ptr(), block_table.data_ptr(), free_list.data_ptr(), free_count.data_ptr(),
                       0 if slot_map is None else slot_map.data_ptr(), new_len.data_ptr(), dev_status.data_ptr(), extra, width)
-    st = load_library().tf_cache_plan(dims.ref, args, _stream(stream))
+    st = load_library().tf_cache_plan(dims.ref, args, _stream_on(stream, gpu))
     if st:
         _check("tf_cache_plan", st)
 
@@ -517,7 +522,7 @@ def tf_cache_append(dims: CacheDims, k, v, slot_map, src, k_cache, v_cache, k_sc
     args = _APPEND.pack(k.data_ptr(), v.data_ptr(), k_row, v_row, slot_map.data_ptr(), 0 if src is None else src.data_ptr(),
                         k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), dev_status.data_ptr(), n,
                         slots[1])
-    st = load_library().tf_cache_append(dims.ref, args, _stream(stream))
+    st = load_library().tf_cache_append(dims.ref, args, _stream_on(stream, gpu))
     if st:
         _check("tf_cache_append", st)
 
@@ -569,7 +574,7 @@ def tf_tree_attention(dims: CacheDims, q, k, v, k_cache, v_cache, k_scale, v_sca
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, k_row, v_row, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(),
         v_scale.data_ptr(), block_table.data_ptr(), seq_len.data_ptr(), 0 if mask is None else mask.data_ptr(), out.data_ptr(),
         0 if lse is None else lse.data_ptr(), dev_status.data_ptr(), ws.data_ptr(), ws.numel(), scale, n)
-    st = load_library().tf_tree_attention(dims.ref, args, _stream(stream))
+    st = load_library().tf_tree_attention(dims.ref, args, _stream_on(stream, gpu))
     if st:
         _check("tf_tree_attention", st)
 
@@ -596,6 +601,6 @@ def tf_sample(logits, u, tok, logp=None, temperature=None, top_k=None, top_p=Non
             (min_p is None or min_p.get_device() == gpu) and gpu == torch.cuda.current_device()):
         _blame_device(("logits", logits), ("u", u), ("tok", tok), ("logp", logp), ("temperature", temperature), ("top_k", top_k),
                       ("top_p", top_p), ("min_p", min_p))
-    status = load_library().tf_sample(args, _stream(stream))
+    status = load_library().tf_sample(args, _stream_on(stream, gpu))
     if status:
         _check("tf_sample", status)
