@@ -411,7 +411,8 @@ typedef struct {
     int32_t batch;        /* b, 1..4096 */
     int32_t heads;        /* query heads, a multiple of kv_heads */
     int32_t kv_heads;     /* heads of keys and values; query head h reads head h / (heads / kv_heads) */
-    int32_t head_dim;     /* a multiple of 16, 16..256 */
+    int32_t head_dim;     /* a multiple of 16, 16..256; with bf16 queries 64 and 128 have tensor-core kernels, other sizes and
+                             fp32 are computed on the CUDA cores */
     int32_t page;         /* tokens per page: 16, 32, 64 or 128 */
     int32_t n_pages;      /* pages of the pool, n_pages * page < 2^31 */
     int32_t max_pages;    /* entries per sequence of the block table, max_pages * page <= 2^31 - 1024 */
@@ -497,7 +498,8 @@ typedef struct {
     int32_t* dev_status;        /* [b] in/out (OR-ed): TF_DEV_BAD_PAGE (a page id outside the pool: its tokens are left
                                    out), TF_DEV_BAD_LENGTH (seq_len outside 0..max_pages * page: taken as the nearest
                                    bound), TF_DEV_TIMEOUT in the first word (a bounded wait gave up; outputs invalid) */
-    void* ws;                   /* tf_attention_workspace_size bytes, 256-byte aligned */
+    void* ws;                   /* tf_attention_workspace_size bytes, 256-byte aligned; in use until the call's kernels have
+                                   finished, so calls on streams that run at once need one each */
     size_t ws_bytes;
     float scale;                /* of the scores, finite and > 0 (1 / sqrt(head_dim) as a rule) */
     int32_t n;

@@ -18,7 +18,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // numerators a lane is every 32nd element of the head. Keys and values are widened to fp32 in shared memory once per
 // tile; the keys' rows are padded by four floats, so that the eight lanes of a 16-byte phase meet eight different
 // groups of banks. Bounded by shared-memory reads (fp32 has no tensor-core form at full precision), for short contexts by latency: 13
-// nodes over 777 tokens of 2 sequences, 16 heads of 64: 21 us with the joining; 4000 tokens: 47 us, 9 TFLOP/s.
+// nodes over 777 tokens of 2 sequences, 16 heads of 64: 22 us with the joining; 4000 tokens: 47 us, 9 TFLOP/s. In bf16 it takes the head
+// sizes other than 64 and 128: one token of 64 sequences with up to 32768 cached, size 96, 2.3 ms, 0.7 TB/s.
 constexpr int kRows = 16, kTok = 32, kWarps = 4, kRowsPerWarp = kRows / kWarps;   // (a float4 holds a token's weights for a warp)
 
 template <typename T>
@@ -352,7 +353,7 @@ cudaError_t launch_simt(cudaStream_t st, const AttnArgs& a, const AttnSplit& p, 
 }
 
 // From 17 rows on the tensor cores' tiles of 128 rows: the kernel for few rows takes 16 at once and would read the cache again
-// for every 16 more. 20 rows over 16 sequences of up to 16384 tokens: 90 us there, 156 here. (Over one of 2000 tokens the two are
+// for every 16 more. 20 rows over 16 sequences of up to 16384 tokens: 92 us there, 162 here. (Over one of 2000 tokens the two are
 // near each other, 18 and 16 us; lengths are not known on the host.)
 bool many_rows(const CacheShape& c, int n) { return static_cast<long long>(n) * c.group > 16 && attn_tiles_take(c); }
 

@@ -20,9 +20,10 @@
 // which keeps f16's 11 bits down to 2^-27 of the largest term of the output. m and sh are whole numbers: what is summed so far
 // is moved by powers of two, without rounding.
 //
-// Bounded by HBM: one token of 64 sequences with up to 32768 cached (32 heads on 8, size 128; 2.15 GB) takes 348 us, 6.2 TB/s, with
-// two CTAs per SM and 255 registers; three at 168 registers spill and take 594. One sequence with 4100 cached: 10.6 us, a chain of
-// page ids, scales and bytes, then the joining.
+// Bounded by HBM: one token of 64 sequences with up to 32768 cached (32 heads on 8, size 128; 2.15 GB) takes 349 us, 6.2 TB/s, with
+// two CTAs per SM and 250 registers; three at 168 registers spill and take 597. (With 9 to 16 rows of size 128 even 255 are too few: 104
+// bytes are spilled; four tokens of the same sequences take 542 us.) One sequence with 4100 cached: 10.6 us, a chain of page ids,
+// scales and bytes, then the joining.
 #include <cuda_fp16.h>
 #include <math.h>
 

@@ -20,10 +20,11 @@
 //   warps 2, 3   values from e4m3 to f16; what lies behind the last token becomes 0
 //   warps 4..19  softmax: four threads per row, 32 columns of S each, which exchange their maxima through shared memory
 // O is rescaled only when a row's largest P would pass 2^15, and m moves only when a score passes it by more than 20 (in log2).
-// Bounded by the softmax warps' instructions and the chain from S to the next P: 2400 cycles per 128 rows and 128 tokens of 128
-// elements, of which the tensor cores need 1100. Trees of 65 nodes of 16 sequences with 1000 to 16384 cached, 32 heads on 8: 261 us,
-// 570 TFLOP/s of what is asked for (their 260 rows per head of keys take three tiles of 128; 64 nodes, two tiles: 194 us). Products issued by
-// two warps, or values widened by one warp or by four at 80 registers: 314 us.
+// Bounded by the softmax warps' instructions and the chain from S to the next P: 2600 cycles per 128 rows and 128 tokens of 128
+// elements, of which the tensor cores need 1100. Trees of 65 nodes of 16 sequences with 1000 to 16384 cached, 32 heads on 8: 284 us,
+// 524 TFLOP/s of what is asked for (their 260 rows per head of keys take three tiles of 128; 64 nodes, two tiles: 210 us). Weights
+// whose sum shared the values' exponent took 261 us, but their sum depended on the values' scales. At that time products
+// issued by two warps, or values widened by one warp or by four at 80 registers, took 314 us.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -735,7 +736,9 @@ __global__ void __launch_bounds__(WideCfg<HD>::kThreads, 1) wide_attention_kerne
 // that one wait for memory covers them all. Bounded by latency.
 // Many items: a CTA's four warps take 16 rows each. Few (SPREAD): all four take the same 16 rows, each every fourth 16 of the new tokens,
 // and then four rows each of the pieces, which are then one wait for memory instead of five: 65 nodes of one sequence over 2000
-// cached tokens take 23.6 us with it and 28.1 without, 9 nodes 18.1 and 24.8.
+// cached tokens take 24.6 us with it and 29.0 without, 9 nodes 18.9 and 25.7.
+// A prompt of 1024 tokens of one sequence, all of whose work is here, takes 176 us, 49 TFLOP/s: chunks are filled without anything
+// in flight for the next one.
 constexpr int kJoinWarps = 4;
 
 __device__ __forceinline__ void mma_bf16_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {

@@ -15,7 +15,7 @@ namespace {
 // 2048 tokens with 8 MB of slots, 15 us.
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanSlots = 2048;         // slots that the same CTA writes; more have a grid of their own. A change and its way back: 1088
-                                         // slots 7.6 us (8.2 in a grid), 3400 slots 8.9 (8.4), 17000 slots 14.0 (9.0), 2 M slots 543 (15)
+                                         // slots 8.1 us (8.5 in a grid), 3400 slots 9.4 (8.6), 17000 slots 14.8 (10.1), 2 M slots 539 (15.5)
 
 struct Change {
     int len, want, have, need, status;   // lengths now and wanted, pages now and wanted
